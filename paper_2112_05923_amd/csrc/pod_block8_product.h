@@ -215,18 +215,36 @@ __device__ inline void hold(f32x16 (&acc)[4]) {
   for (int f = 0; f < 4; ++f) asm volatile("" : "+v"(acc[f]));
 }
 
-// tanh is monotonic: a block's largest |tanh| is that of its largest |sum|, which is known before any of them;
-// 2^-e tanh(z) = 2^-e - 2 2^-e / (e^2z + 1) is then one operation behind the reciprocal.  (Where the two signs of a value round
-// differently a scaled value can lie a last bit above 448, and is 448.)
-__device__ inline int tanh_exponent(const f32x16 (&acc)[4]) {
-  float m = 0.0f;  // (a maximum ignores NaN by itself, and infinite sums have finite values)
-#pragma unroll
-  for (int i = 0; i < 64; ++i) m = fmaxf(m, fabsf(acc[i >> 4][i & 15]));
-  m = __uint_as_float(max_of_two(__float_as_uint(m)));
-  return exponent_of(__float_as_uint(tile::tanh_from_scaled(m * tile::kTwoLog2e)) & 0x7fffffffu);
+// tanh z = 1 - 2 / (e^2z + 1) is off by up to 2^-22 of ONE, whatever z: e^2z + 1 has no digits of a small z.  A result that is
+// rounded to bf16 is therefore z itself below 2^-7, off by z^2 / 3, at most 2.1e-5 of it; from there on 2^-22 is at most 3.1e-5
+// of it (bf16's own rounding: 3.9e-3).  Two operations an entry: 65536 x 1024 x 1024 90 -> 92 us, 64 agents x 1000 x 301 x 256
+// 29 -> 30.5 us; a branch would hardly ever be left out, 64 sums of 32 rows have a small one nearly always.
+constexpr float kTanhIsItself = 0.0078125f;
+__device__ inline float tanh_to_bf16(float z) {
+  const float t = tile::tanh_from_scaled(z * tile::kTwoLog2e);
+  return fabsf(z) < kTanhIsItself ? z : t;
 }
 
-// One row's 64 sums to codes.
+// Blocks whose sums all lie below 1/2 keep the relative precision of their smallest entries with the odd Taylor polynomial up to
+// z^9 (9e-6 of the value at 1/2).  In a block with a larger sum 2^-22 is at most an eighth of half the smallest step of its codes.
+// (A branch by rows: 262144 x 512 x 512 with larger sums as before it.)
+constexpr float kSmallSums = 0.5f;
+__device__ inline float tanh_small(float z) {
+  const float z2 = z * z;
+  return fmaf(z2 * z, fmaf(z2, fmaf(z2, fmaf(z2, 62.0f / 2835.0f, -17.0f / 315.0f), 2.0f / 15.0f), -1.0f / 3.0f), z);
+}
+
+// A row's 2 x 64 sums: the largest |sum|, in both lanes.  (A maximum ignores NaN by itself, and infinite sums have finite tanh.)
+__device__ inline float largest_sum(const f32x16 (&acc)[4]) {
+  float m = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 64; ++i) m = fmaxf(m, fabsf(acc[i >> 4][i & 15]));
+  return __uint_as_float(max_of_two(__float_as_uint(m)));
+}
+
+// One row's 64 sums to codes.  tanh is monotonic: a block's largest |tanh| is that of its largest |sum|, which is known before
+// any of them; from 1/2 on 2^-e tanh(z) = 2^-e - 2 2^-e / (e^2z + 1) is then one operation behind the reciprocal.  (A value may
+// be rounded to 2^-20 of itself above the largest one's: 448 still.)
 __device__ inline void encode_sums(const f32x16 (&acc)[4], bool act, uint32_t (&codes)[16], uint32_t &byte) {
   if (!act) {
     float v[64];
@@ -235,8 +253,21 @@ __device__ inline void encode_sums(const f32x16 (&acc)[4], bool act, uint32_t (&
     encode64(v, codes, byte);
     return;
   }
-  const int e = tanh_exponent(acc);
+  const float m = largest_sum(acc);
+  const bool small = m < kSmallSums;
+  const int e = exponent_of(__float_as_uint(small ? tanh_small(m) : tile::tanh_from_scaled(m * tile::kTwoLog2e)));
   const float inv = power(-e), minus2 = -2.0f * inv;
+  byte = (uint32_t)(e + 127);
+  if (small) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      float v[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = tanh_small(acc[i >> 2][4 * (i & 3) + j]) * inv;
+      codes[i] = codes4(v[0], v[1], v[2], v[3]);
+    }
+    return;
+  }
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     float v[4];
@@ -245,11 +276,11 @@ __device__ inline void encode_sums(const f32x16 (&acc)[4], bool act, uint32_t (&
       v[j] = fmaf(minus2, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(acc[i >> 2][4 * (i & 3) + j] * tile::kTwoLog2e) + 1.0f), inv);
     codes[i] = codes4(v[0], v[1], v[2], v[3]);
   }
-  byte = (uint32_t)(e + 127);
 }
+// A value by itself (of a block too: few rows, whose largest value is found behind the activation).
 template <int OUT>
 __device__ inline float activate(float z, bool act) {
-  return !act ? z : OUT == PR_B8_F32 ? tile::tanh_accurate(z) : tile::tanh_from_scaled(z * tile::kTwoLog2e);
+  return !act ? z : OUT == PR_B8_BF16 ? tanh_to_bf16(z) : tile::tanh_accurate(z);
 }
 
 // Activation and the way out of one row's 64 sums.  All lanes have to come here (blocks: two of them share a maximum).
