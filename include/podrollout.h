@@ -320,7 +320,9 @@ int ppo_learner_step(void *hip_stream, const pr_ppo_config *cfg, const float *ob
  * scale byte = e + 127; the entry stands for q 2^e.  Infinities and NaN become NaN, and only they: the block's other entries
  * are stored as if they were not there.  Weights [in, out] are stored alike in blocks of 128 x 128, packed for the products.
  * Codes must be 16-byte aligned; plain rows (fp32 or bf16, ld elements apart) need only the alignment of their elements.
- * All calls are stateless, only enqueue on hip_stream and allocate nothing. */
+ * All calls are stateless, only enqueue on hip_stream and allocate nothing.  Nothing that a call writes (codes, scale bytes, rows,
+ * gradients, packed weights, workspace) may share a byte with anything else that it writes or reads, or the call is refused
+ * with PR_EINVAL; rows that lie between each other's (columns of one buffer) are fine. */
 enum { PR_B8_F32 = 0, PR_B8_BF16 = 1, PR_B8_BLOCKS = 2 };  /* kinds of rows */
 
 /* x [rows, ldx] of kind PR_B8_F32 or PR_B8_BF16 -> blocks, and back (rounded to bf16: exact).  0 <= rows <= 2^30, 1 <= cols <= 2^20,
@@ -356,7 +358,7 @@ int block8_linear(void *hip_stream, const pr_block8_layer *layer, int32_t x_kind
  * bf16) the gradient of the outputs and Y the values of y's blocks:
  *   g = bf16(fl32(dy fl32(1 - Y^2))), or bf16(dy) without tanh;   dx = g W^T;   dW = X^T g;   db = sum over rows of g
  * (the rounding to blocks is passed straight through; g is the one rounding of gradients).  dx [P rows, lddx] of dx_kind, or
- * NULL; dW [P, in, out], db [P, out] fp32.  dx and dy may not overlap.  Sums run in a fixed order.  rows = 0 gives zeros.
+ * NULL; dW [P, in, out], db [P, out] fp32.  Sums run in a fixed order.  rows = 0 gives zeros.
  * workspace: device, 256-byte aligned, block8_workspace_bytes of it (0 bytes and NULL are fine then). */
 int block8_workspace_bytes(const pr_block8_layer *layer, size_t *out);
 int block8_linear_grads(void *hip_stream, const pr_block8_layer *layer, int32_t dy_kind, const void *dy, int64_t lddy,

@@ -8,6 +8,9 @@
 #include <stdlib.h>
 #include <string.h>
 
+#include <initializer_list>
+#include <numeric>
+
 #include "pod_block8.h"
 #include "pod_internal.h"
 
@@ -727,6 +730,43 @@ bool b8_rows_ok(int32_t kind, const void *p, int64_t ld, int32_t cols, bool empt
 
 bool b8_blocks_ok(const uint8_t *q, const uint8_t *scale, bool empty) { return empty || (b8_aligned(q, 16) && scale); }
 
+// Memory that a call reads or writes: rows of `bytes` bytes, `pitch` bytes apart.
+struct B8Span {
+  const void *at;
+  int64_t rows, pitch, bytes;
+};
+B8Span b8_bytes(const void *p, size_t bytes) { return {p, bytes > 0, 0, (int64_t)bytes}; }
+B8Span b8_plain(int32_t kind, const void *p, int64_t rows, int64_t ld, int32_t cols) {
+  const int64_t size = kind == PR_B8_F32 ? 4 : 2;
+  return {p, rows, ld * size, cols * size};
+}
+B8Span b8_codes(const void *q, int64_t rows, int32_t cols) { return b8_bytes(q, (size_t)rows * ((cols + 127) / 128) * 128); }
+B8Span b8_scales(const void *s, int64_t rows, int32_t cols) { return b8_bytes(s, (size_t)rows * ((cols + 127) / 128)); }
+
+// Rows between each other's (columns of one buffer) share no byte: their places within the largest distance that both pitches are
+// multiples of do not touch.
+bool b8_meet(const B8Span &a, const B8Span &b) {
+  if (!a.at || !b.at || a.rows == 0 || b.rows == 0) return false;
+  const uintptr_t pa = reinterpret_cast<uintptr_t>(a.at), pb = reinterpret_cast<uintptr_t>(b.at);
+  if ((__int128)pa + (__int128)(a.rows - 1) * a.pitch + a.bytes <= pb || (__int128)pb + (__int128)(b.rows - 1) * b.pitch + b.bytes <= pa)
+    return false;
+  const int64_t unit = std::gcd(a.rows > 1 ? a.pitch : 0, b.rows > 1 ? b.pitch : 0);
+  if (unit == 0) return true;
+  const int64_t apart = (int64_t)(pb >= pa ? (pb - pa) % unit : (unit - (int64_t)((pa - pb) % unit)) % unit);
+  return apart < a.bytes || unit - apart < b.bytes;
+}
+
+// Nothing that a call writes may be read by it too, or be written twice: workgroups run in any order.
+bool b8_apart(std::initializer_list<B8Span> written, std::initializer_list<B8Span> read) {
+  for (const B8Span *w = written.begin(); w != written.end(); ++w) {
+    for (const B8Span *o = w + 1; o != written.end(); ++o)
+      if (b8_meet(*w, *o)) return false;
+    for (const B8Span &r : read)
+      if (b8_meet(*w, r)) return false;
+  }
+  return true;
+}
+
 int b8_layer_ok(const pr_block8_layer *l) {
   if (!l || l->n_agents < 1 || l->n_agents > 65535 || l->in_dim < 1 || l->in_dim > kB8MostCols || l->out_dim < 1 ||
       l->out_dim > kB8MostCols || (l->tanh != 0 && l->tanh != 1) || l->rows < 0)
@@ -746,6 +786,7 @@ int block8_quantize(void *hip_stream, int64_t rows, int32_t cols, int32_t kind, 
   if (!b8_rows_ok(kind, x, ldx, cols, rows == 0) || !b8_blocks_ok(q, scale, rows == 0)) return PR_EINVAL;
   if (rows > kB8MostRows) return PR_EUNSUPPORTED;
   if (rows == 0) return PR_OK;
+  if (!b8_apart({b8_codes(q, rows, cols), b8_scales(scale, rows, cols)}, {b8_plain(kind, x, rows, ldx, cols)})) return PR_EINVAL;
   POD_HIP(launch_block8_store(static_cast<hipStream_t>(hip_stream), rows, cols, kind, x, ldx, q, scale));
   return PR_OK;
 }
@@ -756,6 +797,7 @@ int block8_dequantize(void *hip_stream, int64_t rows, int32_t cols, const uint8_
   if (!b8_rows_ok(kind, y, ldy, cols, rows == 0) || !b8_blocks_ok(q, scale, rows == 0)) return PR_EINVAL;
   if (rows > kB8MostRows) return PR_EUNSUPPORTED;
   if (rows == 0) return PR_OK;
+  if (!b8_apart({b8_plain(kind, y, rows, ldy, cols)}, {b8_codes(q, rows, cols), b8_scales(scale, rows, cols)})) return PR_EINVAL;
   POD_HIP(launch_block8_restore(static_cast<hipStream_t>(hip_stream), rows, cols, q, scale, kind, y, ldy));
   return PR_OK;
 }
@@ -774,6 +816,7 @@ int block8_pack_weights(void *hip_stream, const pr_block8_layer *layer, const fl
   if (rc != PR_OK) return rc;
   if (!b8_aligned(W, 4) || !b8_aligned(packed, 256)) return PR_EINVAL;
   if (packed_bytes < need) return PR_ENOMEM;
+  if (!b8_apart({b8_bytes(packed, need)}, {b8_bytes(W, (size_t)layer->n_agents * layer->in_dim * layer->out_dim * 4)})) return PR_EINVAL;
   POD_HIP(launch_block8_pack(static_cast<hipStream_t>(hip_stream), layer->n_agents, layer->in_dim, layer->out_dim, W, packed));
   return PR_OK;
 }
@@ -791,6 +834,16 @@ int block8_linear(void *hip_stream, const pr_block8_layer *layer, int32_t x_kind
     return PR_EINVAL;
   if (!b8_aligned(packed, 256) || (bias && !b8_aligned(bias, 4))) return PR_EINVAL;
   if (empty) return PR_OK;
+  const int64_t rows = layer->n_agents * layer->rows;
+  const bool xb = x_kind == PR_B8_BLOCKS, yb = y_kind == PR_B8_BLOCKS;
+  size_t weights = 0;
+  block8_weight_bytes(layer, &weights);
+  if (!b8_apart({yb ? b8_codes(y, rows, layer->out_dim) : b8_plain(y_kind, y, rows, ldy, layer->out_dim),
+                 b8_scales(yb ? y_scale : nullptr, rows, layer->out_dim)},
+                {xb ? b8_codes(x, rows, layer->in_dim) : b8_plain(x_kind, x, rows, ldx, layer->in_dim),
+                 b8_scales(xb ? x_scale : nullptr, rows, layer->in_dim), b8_bytes(packed, weights),
+                 b8_bytes(bias, (size_t)layer->n_agents * layer->out_dim * 4)}))
+    return PR_EINVAL;
   const Block8Linear a = {layer->n_agents, layer->in_dim, layer->out_dim, layer->tanh, layer->rows, x_kind, x, x_scale, ldx,
                           packed, bias, y_kind, y, y_scale, ldy};
   POD_HIP(launch_block8_linear(static_cast<hipStream_t>(hip_stream), a));
@@ -818,6 +871,16 @@ int block8_linear_grads(void *hip_stream, const pr_block8_layer *layer, int32_t 
   if (!b8_aligned(packed, 256) || !b8_aligned(dW, 4) || !b8_aligned(db, 4)) return PR_EINVAL;
   if (need > 0 && !b8_aligned(workspace, 256)) return PR_EINVAL;
   if (workspace_bytes < need) return PR_ENOMEM;
+  const int64_t rows = layer->n_agents * layer->rows;
+  const size_t biases = (size_t)layer->n_agents * layer->out_dim * 4;
+  size_t weights = 0;
+  block8_weight_bytes(layer, &weights);
+  if (!b8_apart({b8_plain(dx_kind, dx, rows, lddx, layer->in_dim), b8_bytes(dW, biases * layer->in_dim), b8_bytes(db, biases),
+                 b8_bytes(workspace, need)},
+                {b8_plain(dy_kind, dy, rows, lddy, layer->out_dim), b8_codes(y, rows, layer->out_dim),
+                 b8_scales(layer->tanh ? y_scale : nullptr, rows, layer->out_dim), b8_codes(x, rows, layer->in_dim),
+                 b8_scales(x_scale, rows, layer->in_dim), b8_bytes(packed, weights)}))
+    return PR_EINVAL;
   const Block8Grads a = {layer->n_agents, layer->in_dim, layer->out_dim, layer->rows, dy_kind, dy, lddy, y, y_scale, x, x_scale,
                          packed, dx_kind, dx, lddx, dW, db, static_cast<float *>(workspace)};
   POD_HIP(launch_block8_grads(static_cast<hipStream_t>(hip_stream), a));

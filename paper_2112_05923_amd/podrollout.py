@@ -620,7 +620,7 @@ def _blocks_arg(b: Blocks8, shape, device, name):
 
 def block8_linear(x, w: Weights8, bias: Optional[torch.Tensor] = None, tanh: bool = True, out=torch.float32):
     """act(x W + b) on 8-bit blocks.  x: Blocks8 or plain rows [(P,) rows, in]; out: "blocks", torch.float32, torch.bfloat16,
-    or a Blocks8 or tensor to write to."""
+    or a Blocks8 or tensor to write to, which shares no memory with what is read."""
     lead, size, device = w.lead, x.shape, w.device
     if len(size) != len(lead) + 2 or size[:-2] != lead or size[-1] != w.in_dim:
         raise ValueError(f"x: rows of {tuple(size)} for weights of {tuple(lead) + (w.in_dim, w.out_dim)}")
