@@ -692,18 +692,19 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void linear_plain_kernel(Pro
 }
 
 template <class T, bool IN8, int OUT>
-void launch_plain(hipStream_t st, int32_t P, const Product &a) {
+hipError_t launch_plain(hipStream_t st, int32_t P, const Product &a) {
   const int64_t tiles = (a.rows + kPlainRows - 1) / kPlainRows;
   auto go = [&](auto kernel, int obs, int waves) {
     const int32_t groups = (a.nob + obs - 1) / obs;
     hipLaunchKernelGGL(kernel, dim3((unsigned)((tiles + 7) / 8 * 8 * groups), 1, P), dim3(64 * waves), 0, st, a, (int32_t)tiles, groups);
+    return hipGetLastError();
   };
   // the more features share a workgroup the less often rows are encoded, unless that leaves compute units without one
   auto fills = [&](int obs) { return a.nob > obs / 2 && tiles * P * ((a.nob + obs - 1) / obs) >= compute_units(); };
   if constexpr (!IN8)
     if (fills(4)) return go(linear_plain_kernel<T, IN8, OUT, 8, 2>, 4, 8);
-  if (fills(2)) go(linear_plain_kernel<T, IN8, OUT, 8, 1>, 2, 8);
-  else go(linear_plain_kernel<T, IN8, OUT, 4, 1>, 1, 4);
+  if (fills(2)) return go(linear_plain_kernel<T, IN8, OUT, 8, 1>, 2, 8);
+  return go(linear_plain_kernel<T, IN8, OUT, 4, 1>, 1, 4);
 }
 
 // Input gradients of many rows.  A wavefront forms g for its 32 rows and up to 128 NB outputs of the layer once, in registers
@@ -893,23 +894,23 @@ bool launch_input_grads(hipStream_t st, int32_t P, const Product &a) {
 }
 
 template <int SRC, bool IN8, int OUT>
-void launch_rows(hipStream_t st, int32_t P, const Product &a) {
+hipError_t launch_rows(hipStream_t st, int32_t P, const Product &a) {
   if constexpr (SRC == kGradF32 || SRC == kGradBf16)
-    if (launch_input_grads<std::conditional_t<SRC == kGradF32, float, uint16_t>, OUT>(st, P, a)) return;
+    if (launch_input_grads<std::conditional_t<SRC == kGradF32, float, uint16_t>, OUT>(st, P, a)) return hipGetLastError();
   if constexpr (SRC == kBlocks)
     if (!few_rows(P, a.rows) && lines_fit(a)) {
       // Resident weights are paid for at the start: with several blocks of features by the second tile of a workgroup's rows only
       // (to bf16, resident and in tiles: 5000 x 512 x 512 17 and 12.5 us, 26861 x 256 x 256 15 and 12.4, 60000 x 256 x 256 17.8
       // and 16.5; one block, 20000 x 128 x 128 8.6 and 9.2, 1577 x 256 x 75 10.6 and 13.1)
       if (a.nob == 1 || P * ((a.rows + 255) / 256) > compute_units()) {
-        if (a.nib == 1) return (void)launch_resident<IN8, OUT, 1>(st, P, a);
-        if (a.nib == 2) return (void)launch_resident<IN8, OUT, 2>(st, P, a);
-        if (a.nib == 3) return (void)launch_resident<IN8, OUT, 3>(st, P, a);
-        if (a.nib == 4) return (void)launch_resident<IN8, OUT, 4>(st, P, a);
+        if (a.nib == 1) return launch_resident<IN8, OUT, 1>(st, P, a);
+        if (a.nib == 2) return launch_resident<IN8, OUT, 2>(st, P, a);
+        if (a.nib == 3) return launch_resident<IN8, OUT, 3>(st, P, a);
+        if (a.nib == 4) return launch_resident<IN8, OUT, 4>(st, P, a);
       }
       const int32_t tiles = (int32_t)((a.rows + kTilesRows - 1) / kTilesRows);
       hipLaunchKernelGGL((linear_tiles_kernel<IN8, OUT>), dim3((unsigned)((tiles + 7) / 8 * 8 * a.nob), 1, P), dim3(256), 0, st, a, tiles);
-      return;
+      return hipGetLastError();
     }
   bool few = few_rows(P, a.rows);
   if constexpr (SRC == kF32 || SRC == kBf16) {
@@ -921,22 +922,23 @@ void launch_rows(hipStream_t st, int32_t P, const Product &a) {
   if (few) {
     const int split = OUT == PR_B8_BLOCKS ? 1 : 4;
     hipLaunchKernelGGL((linear_few_kernel<SRC, IN8, OUT>), dim3((unsigned)((a.rows + 31) / 32), a.nob * split, P), dim3(1024), 0, st, a);
-    return;
+    return hipGetLastError();
   }
   hipLaunchKernelGGL((linear_kernel<SRC, IN8, OUT>), dim3((unsigned)((a.rows + 127) / 128), a.nob, P), dim3(256), 0, st, a);
+  return hipGetLastError();
 }
 
 template <int SRC>
-void launch_out(hipStream_t st, int32_t P, const Product &a, int32_t y_kind) {
-  if (y_kind == PR_B8_F32) launch_rows<SRC, false, PR_B8_F32>(st, P, a);
-  if (y_kind == PR_B8_BF16) launch_rows<SRC, true, PR_B8_BF16>(st, P, a);
-  if (y_kind == PR_B8_BLOCKS) launch_rows<SRC, true, PR_B8_BLOCKS>(st, P, a);
+hipError_t launch_out(hipStream_t st, int32_t P, const Product &a, int32_t y_kind) {
+  if (y_kind == PR_B8_F32) return launch_rows<SRC, false, PR_B8_F32>(st, P, a);
+  if (y_kind == PR_B8_BF16) return launch_rows<SRC, true, PR_B8_BF16>(st, P, a);
+  return launch_rows<SRC, true, PR_B8_BLOCKS>(st, P, a);
 }
 
 template <int SRC>
-void launch_back(hipStream_t st, int32_t P, const Product &a, int32_t dx_kind) {
-  if (dx_kind == PR_B8_F32) launch_rows<SRC, false, PR_B8_F32>(st, P, a);
-  if (dx_kind == PR_B8_BF16) launch_rows<SRC, false, PR_B8_BF16>(st, P, a);
+hipError_t launch_back(hipStream_t st, int32_t P, const Product &a, int32_t dx_kind) {
+  if (dx_kind == PR_B8_F32) return launch_rows<SRC, false, PR_B8_F32>(st, P, a);
+  return launch_rows<SRC, false, PR_B8_BF16>(st, P, a);
 }
 
 }  // namespace
@@ -956,10 +958,9 @@ hipError_t launch_block8_linear(hipStream_t st, const Block8Linear &l) {
   a.y = l.y, a.y_scale = l.y_scale, a.ldy = l.y_kind == PR_B8_BLOCKS ? (int64_t)w.nob * kBlock : l.ldy;
   a.x_size = l.x_kind == PR_B8_F32 ? 4 : l.x_kind == PR_B8_BF16 ? 2 : 1;
   a.y_size = l.y_kind == PR_B8_F32 ? 4 : l.y_kind == PR_B8_BF16 ? 2 : 1;
-  if (l.x_kind == PR_B8_BLOCKS) launch_out<kBlocks>(st, l.P, a, l.y_kind);
-  if (l.x_kind == PR_B8_F32) launch_out<kF32>(st, l.P, a, l.y_kind);
-  if (l.x_kind == PR_B8_BF16) launch_out<kBf16>(st, l.P, a, l.y_kind);
-  return hipGetLastError();
+  if (l.x_kind == PR_B8_BLOCKS) return launch_out<kBlocks>(st, l.P, a, l.y_kind);
+  if (l.x_kind == PR_B8_F32) return launch_out<kF32>(st, l.P, a, l.y_kind);
+  return launch_out<kBf16>(st, l.P, a, l.y_kind);
 }
 
 hipError_t launch_block8_input_grads(hipStream_t st, const Block8Grads &l) {
@@ -972,9 +973,8 @@ hipError_t launch_block8_input_grads(hipStream_t st, const Block8Grads &l) {
   a.y = l.dx, a.ldy = l.lddx;
   a.x_size = l.dy_kind == PR_B8_F32 ? 4 : 2;
   a.y_size = l.dx_kind == PR_B8_F32 ? 4 : 2;
-  if (l.dy_kind == PR_B8_F32) launch_back<kGradF32>(st, l.P, a, l.dx_kind);
-  if (l.dy_kind == PR_B8_BF16) launch_back<kGradBf16>(st, l.P, a, l.dx_kind);
-  return hipGetLastError();
+  if (l.dy_kind == PR_B8_F32) return launch_back<kGradF32>(st, l.P, a, l.dx_kind);
+  return launch_back<kGradBf16>(st, l.P, a, l.dx_kind);
 }
 
 }  // namespace pod

@@ -1,0 +1,30 @@
+"""What calls of the 8-bit block layers launch, seen by a process whose HIP runtime only records (launch_recorder)."""
+import shutil
+
+import pytest
+
+from launch_recorder import record
+from paper_2112_05923_amd import podrollout as pr
+
+pytestmark = pytest.mark.skipif(shutil.which("gcc") is None or shutil.which("c++filt") is None, reason="no gcc")
+
+F32, BF16, BLOCKS = pr.PR_B8_F32, pr.PR_B8_BF16, pr.PR_B8_BLOCKS
+X, XS, W, B, Y, YS, DY, DX, DW, DB, WS = ((i + 1) << 44 for i in range(11))  # places far apart that no call touches
+
+
+def linear(rows, ins, outs, x=BLOCKS, y=BLOCKS, agents=1, ldx=None, ldy=None):
+    return ("block8_linear", [0, [agents, ins, outs, 1, rows], x, X, XS, ldx or ins, W, B, y, Y, YS, ldy or outs])
+
+
+def grads(rows, ins, outs, dy=BF16, dx=BF16, tanh=1, agents=1):
+    y = (Y, YS) if tanh else (None, None)
+    return ("block8_linear_grads", [0, [agents, ins, outs, tanh, rows], dy, DY, outs, *y, X, XS, W, dx, DX, ins, DW, DB, WS, 1 << 43])
+
+
+def test_an_error_of_the_runtime_reaches_the_caller():
+    """The resident kernels ask for more LDS than a kernel has by itself; where that is refused the call has not run."""
+    calls = [linear(262144, 512, 512), linear(262144, 512, 30, y=F32), linear(70000, 100, 60, y=BF16)]
+    for c in record(calls):
+        assert c.code == pr.PR_OK and [l.kernel.split("<")[0] for l in c.launches] == ["linear_resident_kernel"]
+    for c in record(calls, RECORDER_REFUSES_ATTRIBUTES="1"):
+        assert c.code == pr.PR_EHIP and not c.launches
