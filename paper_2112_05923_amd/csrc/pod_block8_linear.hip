@@ -11,7 +11,8 @@ namespace b8 {
 namespace {
 
 // A wavefront has 32 rows x 128 features; operands straight from memory.  What the kernels below do not take: rows so far apart
-// that 32 of them span 2 GiB, many plain rows of fewer than 8 entries, gradients of many rows behind more than 1024 outputs.
+// that 32 of them span 2 GiB, many plain rows of fewer than 8 entries or too many for a launch, gradients of many rows behind
+// more than 1024 outputs.
 template <int SRC, bool IN8, int OUT>
 __global__ __launch_bounds__(256) void linear_kernel(Product a) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, ob = blockIdx.y, h = lane >> 5;
@@ -691,6 +692,10 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void linear_plain_kernel(Pro
   for (int t = 0; t < TILES; ++t) finish_lines<OUT>(acc[t], a, row0 + first + 32 * t, ob, lane, rooms[wave]);
 }
 
+// A launch has fewer than 2^32 threads: 2 for each row and block of features here (4 wavefronts for 128 rows and one, 8 for two).
+// With a billion rows of more than one block linear_kernel has them on another axis.
+inline bool plain_fits(const Product &a) { return (a.rows + 8 * kPlainRows) * (a.nob == 1 ? 1 : (a.nob + 1) / 2 * 2) < (int64_t)1 << 31; }
+
 template <class T, bool IN8, int OUT>
 hipError_t launch_plain(hipStream_t st, int32_t P, const Product &a) {
   const int64_t tiles = (a.rows + kPlainRows - 1) / kPlainRows;
@@ -917,7 +922,7 @@ hipError_t launch_rows(hipStream_t st, int32_t P, const Product &a) {
     // (one block of features, and workgroups of 128 rows for less than half of the compute units: 3758 rows of 1261 to 128 outputs
     // in bf16 32 us that way, 21 this; with more features rows are encoded too often, 3000 x 900 x 512 24 us that way, 32 this)
     few = few || (a.nob == 1 && a.nib >= 4 && P * ((a.rows + kPlainRows - 1) / kPlainRows) < compute_units() / 2);
-    if (!few && a.ins >= 8 && lines_fit(a)) return launch_plain<std::conditional_t<SRC == kF32, float, uint16_t>, IN8, OUT>(st, P, a);
+    if (!few && a.ins >= 8 && lines_fit(a) && plain_fits(a)) return launch_plain<std::conditional_t<SRC == kF32, float, uint16_t>, IN8, OUT>(st, P, a);
   }
   if (few) {
     const int split = OUT == PR_B8_BLOCKS ? 1 : 4;

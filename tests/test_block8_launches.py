@@ -28,3 +28,14 @@ def test_an_error_of_the_runtime_reaches_the_caller():
         assert c.code == pr.PR_OK and [l.kernel.split("<")[0] for l in c.launches] == ["linear_resident_kernel"]
     for c in record(calls, RECORDER_REFUSES_ATTRIBUTES="1"):
         assert c.code == pr.PR_EHIP and not c.launches
+
+
+# (what such a call reads and writes is up to 300 GB: the largest cards hold the first four)
+WIDEST = [linear(1 << 30, 8, 256, x=BF16), linear(1 << 30, 8, 129, x=BF16, y=BF16), linear(1 << 29, 8, 257, x=BF16, y=BF16),
+          linear(1 << 29, 8, 512, x=BF16), linear(1 << 30, 5, 128, x=BF16), linear(1 << 30, 8, 128, x=BF16), linear(1 << 30, 128, 128),
+          grads(1 << 30, 128, 8), grads(1 << 30, 64, 64, tanh=0), grads(1000, 65536, 65536), grads(100, 1 << 20, 1 << 15)]
+
+
+def test_the_longest_calls_stay_within_a_launch():
+    for call, got in zip(WIDEST, record(WIDEST)):
+        assert got.code == pr.PR_OK and got.launches, (call, got)
