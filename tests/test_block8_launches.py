@@ -39,3 +39,13 @@ WIDEST = [linear(1 << 30, 8, 256, x=BF16), linear(1 << 30, 8, 129, x=BF16, y=BF1
 def test_the_longest_calls_stay_within_a_launch():
     for call, got in zip(WIDEST, record(WIDEST)):
         assert got.code == pr.PR_OK and got.launches, (call, got)
+
+
+def test_gradients_of_no_rows_are_zeroed_whole():
+    """dW of 2^32 entries too: the launches' threads cover it, and db once."""
+    for agents, ins, outs in ((1, 65536, 65536), (64, 8192, 8192), (1, 70, 30), (3, 20000, 20000)):
+        got, = record([grads(0, ins, outs, agents=agents)])
+        assert got.code == pr.PR_OK
+        entries = agents * (ins + 1) * outs
+        splits = {"join_kernel<1>": 1, "join_kernel<4>": 4, "join_kernel<16>": 16}
+        assert sum(l.grid[0] * l.block[0] // splits[l.kernel] for l in got.launches) >= entries
