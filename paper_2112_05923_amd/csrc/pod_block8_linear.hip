@@ -1,6 +1,7 @@
 // One layer on 8-bit blocks: y = act(x W + b), and with the roles of the weights' sides
 // exchanged the input gradients dx = g W^T of its backward pass (layouts: pod_block8.h).
 #include <algorithm>
+#include <cstddef>
 
 #include "pod_block8.h"
 #include "pod_block8_product.h"
@@ -104,8 +105,10 @@ __global__ __launch_bounds__(1024) void linear_few_kernel(Product a) {
   }
 }
 
-// 64 lanes x 16 bytes from `base` (uniform) + `offset` (a lane's own) straight into LDS (its first 64 KiB: the address's register
-// has 16 bits of it); waited for by arrived().
+// 64 lanes x 16 bytes from `base` (uniform) + `offset` (a lane's own) straight into LDS (its first 64 KiB, kCopyReach: the address's
+// register has 16 bits of it); waited for by arrived().  Kernels that copy have one LDS object, which starts at 0, and what they
+// copy into in front.
+constexpr int kCopyReach = 65536;
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
 __device__ inline void copy_to_lds(const uint8_t *base, uint32_t offset, uint32_t lds) {
@@ -450,7 +453,13 @@ constexpr int kStageBytes = 16384, kRowsBytes = 64 * kBlock;
 template <bool IN8, int OUT>
 __global__ __launch_bounds__(256, 2) void linear_tiles_kernel(Product a, int32_t row_tiles) {
   constexpr int kStages = IN8 ? 1 : 2;  // of a block of inputs
-  __shared__ __attribute__((aligned(16))) uint8_t ring[2][kStageBytes], own[4][kRowsBytes];
+  struct Lds {
+    uint8_t ring[2][kStageBytes], own[4][kRowsBytes];
+  };
+  static_assert(sizeof(Lds) <= kCopyReach, "copies reach all of it");
+  __shared__ __attribute__((aligned(16))) Lds lds;
+  auto &ring = lds.ring;
+  auto &own = lds.own;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, r32 = lane & 31;
   const int i = blockIdx.x >> 3, ob = i % a.nob, tile = i / a.nob * 8 + place_of(blockIdx.x, row_tiles, blockIdx.z);
   if (tile >= row_tiles) return;
@@ -721,7 +730,13 @@ hipError_t launch_plain(hipStream_t st, int32_t P, const Product &a) {
 template <class T, int OUT, int NB>
 __global__ __launch_bounds__(NB <= 4 ? 512 : 256, NB <= 4 ? 2 : 1) void input_grads_kernel(Product a, int32_t slab_blocks) {
   constexpr int kWaves = NB <= 4 ? 8 : 4, kPart = kWideTileBytes / kWaves;
-  __shared__ __attribute__((aligned(16))) uint8_t ring[2][kWideTileBytes], rooms[kWaves][kRoomBytes];
+  struct Lds {
+    uint8_t ring[2][kWideTileBytes], rooms[kWaves][kRoomBytes];
+  };
+  static_assert(offsetof(Lds, rooms) <= kCopyReach, "copies reach the ring");
+  __shared__ __attribute__((aligned(16))) Lds lds;
+  auto &ring = lds.ring;
+  auto &rooms = lds.rooms;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   a.to_agent(blockIdx.z);
   const int64_t row0 = ((int64_t)blockIdx.x * kWaves + wave) * 32;
