@@ -739,6 +739,7 @@ __global__ __launch_bounds__(NB <= 4 ? 512 : 256, NB <= 4 ? 2 : 1) void input_gr
   auto &rooms = lds.rooms;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   a.to_agent(blockIdx.z);
+  a.act = 0;  // (as launched: told here, the way out has no activation to form and leave out)
   const int64_t row0 = ((int64_t)blockIdx.x * kWaves + wave) * 32;
   const uint32_t ring_at = lds_address(&ring[0][0]) + wave * kPart;
   const int ob0 = blockIdx.y * slab_blocks, ob1 = min(ob0 + slab_blocks, a.nob);
