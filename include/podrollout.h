@@ -359,7 +359,8 @@ int block8_linear(void *hip_stream, const pr_block8_layer *layer, int32_t x_kind
  *   g = bf16(fl32(dy fl32(1 - Y^2))), or bf16(dy) without tanh;   dx = g W^T;   dW = X^T g;   db = sum over rows of g
  * (the rounding to blocks is passed straight through; g is the one rounding of gradients).  dx [P rows, lddx] of dx_kind, or
  * NULL; dW [P, in, out], db [P, out] fp32.  Sums run in a fixed order.  rows = 0 gives zeros.
- * workspace: device, 256-byte aligned, block8_workspace_bytes of it (0 bytes and NULL are fine then). */
+ * workspace: device, 256-byte aligned, block8_workspace_bytes of it: a size that serves any call of this layer with up to
+ * `rows` rows (0 bytes and NULL are fine for none). */
 int block8_workspace_bytes(const pr_block8_layer *layer, size_t *out);
 int block8_linear_grads(void *hip_stream, const pr_block8_layer *layer, int32_t dy_kind, const void *dy, int64_t lddy,
                         const uint8_t *y, const uint8_t *y_scale, const uint8_t *x, const uint8_t *x_scale, const void *packed,

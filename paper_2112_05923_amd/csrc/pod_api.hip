@@ -8,6 +8,7 @@
 #include <stdlib.h>
 #include <string.h>
 
+#include <algorithm>
 #include <initializer_list>
 #include <numeric>
 
@@ -778,6 +779,9 @@ int b8_layer_ok(const pr_block8_layer *l) {
   return PR_OK;
 }
 
+// A call with rows has a workspace, of one aligned piece where it puts nothing there.
+size_t b8_workspace(const pr_block8_layer &l, size_t scratch) { return l.rows == 0 ? 0 : std::max<size_t>(scratch, 256); }
+
 }  // namespace
 
 int block8_quantize(void *hip_stream, int64_t rows, int32_t cols, int32_t kind, const void *x, int64_t ldx, uint8_t *q,
@@ -854,16 +858,16 @@ int block8_workspace_bytes(const pr_block8_layer *layer, size_t *out) {
   if (!out) return PR_EINVAL;
   const int rc = b8_layer_ok(layer);
   if (rc != PR_OK) return rc;
-  *out = block8_grads_scratch(layer->n_agents, layer->rows, layer->in_dim, layer->out_dim);
+  *out = b8_workspace(*layer, block8_grads_most_scratch(layer->n_agents, layer->rows, layer->in_dim, layer->out_dim));
   return PR_OK;
 }
 
 int block8_linear_grads(void *hip_stream, const pr_block8_layer *layer, int32_t dy_kind, const void *dy, int64_t lddy,
                         const uint8_t *y, const uint8_t *y_scale, const uint8_t *x, const uint8_t *x_scale, const void *packed,
                         int32_t dx_kind, void *dx, int64_t lddx, float *dW, float *db, void *workspace, size_t workspace_bytes) {
-  size_t need = 0;
-  const int rc = block8_workspace_bytes(layer, &need);
+  const int rc = b8_layer_ok(layer);
   if (rc != PR_OK) return rc;
+  const size_t need = b8_workspace(*layer, block8_grads_scratch(layer->n_agents, layer->rows, layer->in_dim, layer->out_dim));
   const bool empty = layer->rows == 0;
   if (!b8_rows_ok(dy_kind, dy, lddy, layer->out_dim, empty) || !b8_blocks_ok(x, x_scale, empty)) return PR_EINVAL;
   if (layer->tanh ? !b8_blocks_ok(y, y_scale, empty) : y != nullptr) return PR_EINVAL;

@@ -245,7 +245,9 @@ struct Block8Grads {
   float *dW, *db;
   float *parts;
 };
+// Bytes of `parts` for these rows, and for any number of rows up to them.
 size_t block8_grads_scratch(int32_t P, int64_t rows, int32_t in_dim, int32_t out_dim);
+size_t block8_grads_most_scratch(int32_t P, int64_t rows, int32_t in_dim, int32_t out_dim);
 hipError_t launch_block8_grads(hipStream_t st, const Block8Grads &a);
 
 }  // namespace pod

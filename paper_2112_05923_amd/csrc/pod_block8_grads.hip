@@ -267,21 +267,37 @@ struct Plan {
   int32_t tile_k, tile_n, tiles_k, tiles_n, runs;
   int64_t rows;
 };
-constexpr int kTileNarrow = 32, kRunRows = 128;
+constexpr int kTileNarrow = 32, kRunRows = 128, kWorkgroups = 512;
+int64_t tile_plan(Plan &p, int32_t P, int32_t in_dim, int32_t out_dim, int32_t tile_k) {  // how many tiles that makes
+  p.tile_k = tile_k, p.tile_n = out_dim <= kTileNarrow ? kTileNarrow : 128;
+  p.tiles_k = (in_dim + p.tile_k - 1) / p.tile_k, p.tiles_n = (out_dim + p.tile_n - 1) / p.tile_n;
+  return (int64_t)p.tiles_k * p.tiles_n * P;
+}
+int64_t runs_wanted(int64_t tiles, int64_t most) { return std::max<int64_t>(1, std::min(kWorkgroups / tiles, most)); }
 Plan plan_of(int32_t P, int64_t rows, int32_t in_dim, int32_t out_dim) {
-  Plan p = {256, out_dim <= kTileNarrow ? kTileNarrow : 128, 0, 0, 0, 0};
-  auto tiles = [&] {
-    p.tiles_k = (in_dim + p.tile_k - 1) / p.tile_k, p.tiles_n = (out_dim + p.tile_n - 1) / p.tile_n;
-    return (int64_t)p.tiles_k * p.tiles_n * P;
-  };
-  if (rows == 0) return tiles(), p;
+  Plan p = {};
+  int64_t tiles = tile_plan(p, P, in_dim, out_dim, 256);
+  if (rows == 0) return p;
   const int64_t most = (rows + kRunRows - 1) / kRunRows;
-  if (p.tile_n == 128 && (in_dim <= 128 || tiles() * most < 512)) p.tile_k = 128;
-  int64_t want = 512 / tiles();
-  want = want > most ? most : want < 1 ? 1 : want;
+  if (p.tile_n == 128 && (in_dim <= 128 || tiles * most < kWorkgroups)) tiles = tile_plan(p, P, in_dim, out_dim, 128);
+  const int64_t want = runs_wanted(tiles, most);
   p.rows = ((rows + want - 1) / want + kStage - 1) / kStage * kStage;
   p.runs = (int32_t)((rows + p.rows - 1) / p.rows);
   return p;
+}
+// At least the runs of any number of rows up to `rows` (more rows have fewer runs where they take the larger tiles).
+int64_t most_runs(int32_t P, int64_t rows, int32_t in_dim, int32_t out_dim) {
+  if (rows == 0) return 0;
+  Plan p = {};
+  const int64_t most = (rows + kRunRows - 1) / kRunRows, large = tile_plan(p, P, in_dim, out_dim, 256);
+  if (p.tile_n != 128) return runs_wanted(large, most);
+  const int64_t small = tile_plan(p, P, in_dim, out_dim, 128);
+  if (in_dim <= 128) return runs_wanted(small, most);
+  const int64_t in_small_tiles = std::min((kWorkgroups - 1) / large, most);  // parts of rows that small tiles are taken for
+  return std::max(runs_wanted(small, in_small_tiles), in_small_tiles < most ? runs_wanted(large, most) : 1);
+}
+size_t scratch_of(int64_t runs, int32_t P, int32_t in_dim, int32_t out_dim) {
+  return runs > 1 ? (size_t)runs * P * ((size_t)in_dim * out_dim + out_dim) * 4 : 0;
 }
 
 template <class T>
@@ -309,8 +325,12 @@ void launch_weight_grads(hipStream_t st, const WeightGrads &d, const Plan &p) {
 
 using namespace b8;
 
+// (a single run's sums are the results themselves)
 size_t block8_grads_scratch(int32_t P, int64_t rows, int32_t in_dim, int32_t out_dim) {
-  return (size_t)plan_of(P, rows, in_dim, out_dim).runs * P * ((size_t)in_dim * out_dim + out_dim) * 4;
+  return scratch_of(plan_of(P, rows, in_dim, out_dim).runs, P, in_dim, out_dim);
+}
+size_t block8_grads_most_scratch(int32_t P, int64_t rows, int32_t in_dim, int32_t out_dim) {
+  return scratch_of(most_runs(P, rows, in_dim, out_dim), P, in_dim, out_dim);
 }
 
 hipError_t launch_block8_grads(hipStream_t st, const Block8Grads &l) {

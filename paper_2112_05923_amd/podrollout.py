@@ -656,6 +656,7 @@ def block8_linear(x, w: Weights8, bias: Optional[torch.Tensor] = None, tanh: boo
 
 
 def block8_workspace(w: Weights8, rows: int, device) -> torch.Tensor:
+    """Workspace of block8_linear_grads for up to `rows` rows (of each agent)."""
     n = C.c_size_t(0)
     _check(lib().block8_workspace_bytes(C.byref(w.layer(rows, False)), C.byref(n)), "block8_workspace_bytes")
     return torch.empty(n.value + 256, dtype=torch.uint8, device=device)
