@@ -492,6 +492,8 @@ class Blocks8:
             raise TypeError("blocks: need contiguous cuda tensors, codes of float8_e4m3fn and scale bytes of uint8")
         if q.shape[-1] != 128 * nb or scale.shape != lead + (nb,):
             raise ValueError(f"blocks: codes {tuple(q.shape)} and scales {tuple(scale.shape)} for {cols} columns")
+        if scale.device != q.device:
+            raise ValueError(f"blocks: codes on {q.device} and scales on {scale.device}")
         self.q, self.scale, self.cols, self.shape = q, scale, int(cols), lead + (int(cols),)
 
     @staticmethod
