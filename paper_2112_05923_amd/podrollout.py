@@ -409,7 +409,7 @@ def ppo_workspace(cfg: PrPpoConfig, device) -> torch.Tensor:
 
 def _aligned_ptr(ws: torch.Tensor):
     p = (ws.data_ptr() + 255) // 256 * 256
-    return p, ws.numel() - (p - ws.data_ptr())
+    return p, max(0, ws.numel() - (p - ws.data_ptr()))  # (bytes; a negative number would be a huge one in C)
 
 
 def _batch_args(cfg, obs, act_raw, logp_old, adv, ret, rows):
@@ -677,6 +677,8 @@ def block8_linear_grads(dy: torch.Tensor, x: Blocks8, w: Weights8, y: Optional[B
     ik, ip, lddx = (PR_B8_F32, None, 0) if dx is None else _plain_rows(dx, "dx", ins)[:3]
     if workspace is None:
         workspace = block8_workspace(w, rows, device)
+    elif not workspace.is_contiguous():
+        raise TypeError("workspace: need a contiguous tensor")
     _same_device(device, dy=dy, dx=dx, workspace=workspace)
     dW = torch.empty(lead + (w.in_dim, w.out_dim), dtype=torch.float32, device=device)
     db = torch.empty(lead + (w.out_dim,), dtype=torch.float32, device=device)

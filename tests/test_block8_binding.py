@@ -17,3 +17,12 @@ def test_codes_and_scales_are_on_one_device():
     assert pr.Blocks8(codes, _on("cuda:0", torch.uint8, 4, 2), 200).shape == (4, 200)
     with pytest.raises(ValueError):
         pr.Blocks8(codes, _on("cuda:1", torch.uint8, 4, 2), 200)
+
+
+def test_a_workspace_of_less_than_its_alignment_is_empty():
+    room = torch.empty(1024, dtype=torch.uint8)
+    for at in range(0, 512, 5):
+        for n in (0, 3, 100, 400):
+            part = room[at:at + n]
+            p, left = pr._aligned_ptr(part)
+            assert p % 256 == 0 and left >= 0 and (left == 0 or p + left == part.data_ptr() + n)

@@ -30,3 +30,16 @@ def test_too_little_of_it_is_refused():
     with pytest.raises(pr.PodError) as e:
         pr.block8_linear_grads(dy, xb, weights, workspace=pr.block8_workspace(weights, 200, DEV))
     assert e.value.code == pr.PR_ENOMEM
+
+
+def test_one_that_is_not_there_is_refused():
+    """A byte that stands for many, and the few bytes in front of a boundary."""
+    x, w, _ = _layer(None, 2000, 300, 200, seed=7)
+    weights, xb, dy = pr.Weights8(w.to(DEV)), pr.block8_quantize(x.to(DEV)), _rand((2000, 200), 8).to(DEV)
+    need = pr.block8_workspace(weights, 2000, DEV).numel()
+    with pytest.raises(TypeError):
+        pr.block8_linear_grads(dy, xb, weights, workspace=torch.zeros(1, dtype=torch.uint8, device=DEV).expand(need))
+    short = torch.zeros(512, dtype=torch.uint8, device=DEV)
+    with pytest.raises(pr.PodError) as e:
+        pr.block8_linear_grads(dy, xb, weights, workspace=short[1:9])
+    assert e.value.code == pr.PR_ENOMEM
