@@ -945,7 +945,9 @@ hipError_t launch_rows(hipStream_t st, int32_t P, const Product &a) {
     hipLaunchKernelGGL((linear_few_kernel<SRC, IN8, OUT>), dim3((unsigned)((a.rows + 31) / 32), a.nob * split, P), dim3(1024), 0, st, a);
     return hipGetLastError();
   }
-  hipLaunchKernelGGL((linear_kernel<SRC, IN8, OUT>), dim3((unsigned)((a.rows + 127) / 128), a.nob, P), dim3(256), 0, st, a);
+  // (blocks to blocks have left by now: their rows are close together)
+  if constexpr (SRC != kBlocks || OUT != PR_B8_BLOCKS)
+    hipLaunchKernelGGL((linear_kernel<SRC, IN8, OUT>), dim3((unsigned)((a.rows + 127) / 128), a.nob, P), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 

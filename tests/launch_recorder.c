@@ -24,6 +24,7 @@ void __hipRegisterFunction(void **m, const void *host, char *fn, const char *nam
   if (n_kernels == 4096) abort();
   kernels[n_kernels].host = host;
   snprintf(kernels[n_kernels++].name, sizeof kernels[0].name, "%s", name);
+  if (getenv("RECORDER_LISTS_KERNELS")) printf("kernel %s\n", name);
 }
 int __hipPushCallConfiguration(dim3_t grid, dim3_t block, size_t lds, void *stream) {
   pushed.grid = grid, pushed.block = block, pushed.lds = lds, pushed.stream = stream;

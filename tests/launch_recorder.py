@@ -19,15 +19,29 @@ Launch = collections.namedtuple("Launch", "kernel grid block lds")
 Call = collections.namedtuple("Call", "code launches out")
 
 
-def record(calls, **env):
+def _lines(calls, env):
     with tempfile.TemporaryDirectory() as room:
         runtime = os.path.join(room, "recorder.so")
         subprocess.run(["gcc", "-std=gnu11", "-O1", "-Wall", "-shared", "-fPIC", os.path.join(HERE, "launch_recorder.c"), "-o", runtime], check=True)
         r = subprocess.run([sys.executable, os.path.abspath(__file__), runtime], input=json.dumps(calls), capture_output=True, text=True,
                            timeout=300, env=dict(os.environ, **env))
     assert r.returncode == 0, r.stderr[-2000:]
+    return r.stdout.splitlines()
+
+
+def _readable(names):
+    out = subprocess.run(["c++filt"], input="\n".join(names), capture_output=True, text=True).stdout.split("\n")
+    return [n.replace("void ", "").replace("pod::b8::(anonymous namespace)::", "").split("(")[0] for n in out[:len(names)]]
+
+
+def kernels():
+    """All kernels of the library."""
+    return _readable([l.split()[1] for l in _lines([], {"RECORDER_LISTS_KERNELS": "1"}) if l.startswith("kernel ")])
+
+
+def record(calls, **env):
     got, launches = [], []
-    for line in r.stdout.splitlines():
+    for line in _lines(calls, env):
         word, *rest = line.split()
         if word == "launch":
             n = [int(v) for v in rest[1:]]
@@ -35,8 +49,7 @@ def record(calls, **env):
         elif word == "call":
             got.append(Call(int(rest[0]), launches, int(rest[1])))
             launches = []
-    names = subprocess.run(["c++filt"], input="\n".join(l.kernel for c in got for l in c.launches), capture_output=True, text=True).stdout.split("\n")
-    names = iter(n.replace("void ", "").replace("pod::b8::(anonymous namespace)::", "").split("(")[0] for n in names)
+    names = iter(_readable([l.kernel for c in got for l in c.launches]))
     return [Call(c.code, [l._replace(kernel=next(names)) for l in c.launches], c.out) for c in got]
 
 

@@ -3,7 +3,7 @@ import shutil
 
 import pytest
 
-from launch_recorder import record
+from launch_recorder import kernels, record
 from paper_2112_05923_amd import podrollout as pr
 
 pytestmark = pytest.mark.skipif(shutil.which("gcc") is None or shutil.which("c++filt") is None, reason="no gcc")
@@ -49,3 +49,25 @@ def test_gradients_of_no_rows_are_zeroed_whole():
         entries = agents * (ins + 1) * outs
         splits = {"join_kernel<1>": 1, "join_kernel<4>": 4, "join_kernel<16>": 16}
         assert sum(l.grid[0] * l.block[0] // splits[l.kernel] for l in got.launches) >= entries
+
+
+def test_the_gpu_tests_reach_every_kernel():
+    """The sizes of the tests on a GPU, by the rules of the launches, against the kernels that the library has."""
+    import test_gpu_block8_paths as paths
+    import test_gpu_block8_small as small
+    kinds = {"f32": F32, "bf16": BF16, "blocks": BLOCKS}
+    plain = (F32, BF16)
+    calls = [("block8_quantize", [0, 4, 10, k, X, 10, Y, YS]) for k in plain] + [("block8_dequantize", [0, 4, 10, Y, YS, k, X, 10]) for k in plain]
+    calls.append(("block8_pack_weights", [0, [1, 10, 10, 0, 0], W, Y, 1 << 30]))
+    calls += [linear(*s[:3], kinds[s[3]], y) for s in small.CASES for y in kinds.values()]
+    calls += [linear(*s[1:], x, y, agents=s[0] or 1) for s in paths.PLAIN for x in plain for y in kinds.values()]
+    calls += [linear(*s[1:], BLOCKS, y, agents=s[0] or 1) for s in paths.STORED for y in kinds.values()]
+    calls += [grads(*s[1:], dy, dx, t, agents=s[0] or 1) for s in paths.GRADS for dy in plain for dx in plain for t in (0, 1)]
+    far = {F32: paths.FAR_BYTES // 4, BF16: paths.FAR_BYTES // 2}
+    calls += [linear(paths.FAR_ROWS, 200, 300, x, y, ldx=far.get(x), ldy=far[y]) for x in kinds.values() for y in plain]
+    calls += [(n, [*a[:15], far[k], *a[16:]]) for k in plain for n, a in [grads(paths.FAR_ROWS, 200, 300, k, k)]]
+    got = record(calls)
+    assert all(c.code == pr.PR_OK for c in got), [(a, c) for a, c in zip(calls, got) if c.code != pr.PR_OK][:3]
+    used = {l.kernel for c in got for l in c.launches}
+    mine = {k for k in kernels() if k.startswith(("block8_", "linear_", "input_grads_", "weight_grads_", "join_kernel"))}
+    assert used <= mine and not mine - used, sorted(mine - used)
