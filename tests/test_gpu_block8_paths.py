@@ -1,8 +1,8 @@
 """Every way that layers on 8-bit blocks are computed, held to exact results over all of their rows.
 
 Entries are small whole numbers, and weights of layers 64ths of them: what is stored is stored exactly, and all sums are exact in
-fp32, so sums, gradients and their rounded forms have to be equal bit for bit, and an activation is seen by itself.  The sizes are those at
-which the rules of the launches choose each kernel (test_block8_launches holds the tables to that): rows by the ten thousand,
+fp32, so sums, gradients and their rounded forms have to be equal bit for bit, and an activation is seen by itself.  Blocks have
+scales of their own, a few powers of two apart.  The sizes are those at which the rules of the launches choose each kernel (test_block8_launches holds the tables to that): rows by the ten thousand,
 that leave a ragged tile behind, workgroups that walk several blocks, wavefronts without a block of their own, rows far apart.
 """
 import pytest
@@ -29,6 +29,13 @@ def whole(shape, most, seed):
     gen = torch.Generator(device=DEV)
     gen.manual_seed(seed)
     return torch.randint(-most, most + 1, shape, generator=gen, device=DEV).float()
+
+
+def scales(shape, most, seed, rows=1):
+    """Powers of two up to 2^most and down to 2^-most for each `rows` rows x 128 columns."""
+    lead, (n, cols) = shape[:-2], shape[-2:]
+    e = whole(lead + ((n + rows - 1) // rows, (cols + o.BLOCK - 1) // o.BLOCK), most, seed)
+    return o.power(e).float().repeat_interleave(rows, -2)[..., :n, :].repeat_interleave(o.BLOCK, -1)[..., :cols]
 
 
 def product(a, b):
@@ -66,7 +73,8 @@ def _check_layer(xin, x, weights, w, b):
 
 def _layer(agents, rows, ins, outs):
     lead = () if agents is None else (agents,)
-    return (whole(lead + (rows, ins), 2, rows + ins), whole(lead + (ins, outs), 2, outs) / 64, whole(lead + (outs,), 64, 3) / 64)
+    sx, sw = lead + (rows, ins), lead + (ins, outs)
+    return (whole(sx, 2, rows + ins) * scales(sx, 2, 1), whole(sw, 2, outs) * scales(sw, 2, 2, o.BLOCK) / 64, whole(lead + (outs,), 64, 3) / 64)
 
 
 @pytest.mark.parametrize("kind", TYPES)
@@ -84,8 +92,9 @@ def test_products_of_blocks(shape):
 
 def _case(agents, rows, ins, outs, tanh):
     lead = () if agents is None else (agents,)
-    x, w, dy = whole(lead + (rows, ins), 2, rows), whole(lead + (ins, outs), 2, outs), whole(lead + (rows, outs), 3, ins)
-    y = whole(lead + (rows, outs), 2, rows + 1) / 2 if tanh else None
+    sx, sw, sy = lead + (rows, ins), lead + (ins, outs), lead + (rows, outs)
+    x, w, dy = whole(sx, 2, rows) * scales(sx, 1, 1), whole(sw, 2, outs) * scales(sw, 3, 2, o.BLOCK), whole(sy, 3, ins)
+    y = whole(sy, 2, rows + 1) / 4 * scales(sy, 1, 3).clamp(min=1.0) if tanh else None  # up to 1/2, or to 1
     g = dy if y is None else dy * (1 - y * y)
     turned = lambda t: t.transpose(-1, -2).contiguous()
     return x, w, dy, y, product(g, turned(w)), product(turned(x), g).float(), g.double().sum(-2).float()
@@ -146,3 +155,23 @@ def test_rows_far_apart(room, kind):
         _same(far_dx, dx.float().to(t), "dx")
         _same(got[1], dW, "dW")
         _same(got[2], db, "db")
+
+
+@pytest.mark.parametrize("of_rows,of_weights", [(100, -103), (-100, 97), (55, 50), (-55, -50)])
+@pytest.mark.parametrize("shape", [(48, 300, 200), (1500, 300, 30), (3001, 640, 200), (1500, 5, 130)])
+def test_scales_at_the_far_ends(shape, of_rows, of_weights):
+    """Rows and weights whose scales are far from 1, up and down, with products and gradients of either size."""
+    x, w, b = _layer(None, *shape)
+    dy = whole((shape[0], shape[2]), 3, 5)
+    x, w, b = x * 2.0 ** of_rows, w * 2.0 ** of_weights, b * 2.0 ** (of_rows + of_weights)
+    weights, xb, z = pr.Weights8(w), pr.block8_quantize(x), product(x, w) + b.double()
+    for xin in (x, xb):
+        for kind in TYPES.values():
+            _same(pr.block8_linear(xin, weights, b, False, kind), z.float().to(kind), kind)
+        got, want = pr.block8_linear(xin, weights, b, False, "blocks"), pr.block8_quantize(z.float())
+        _same(got.scale, want.scale, "scale bytes")
+        _same(got.q.float(), want.q.float(), "codes")
+    dx, dW, db = pr.block8_linear_grads(dy, xb, weights, dx=torch.float32)
+    _same(dx, product(dy, w.T.contiguous()).float(), "dx")
+    _same(dW, product(x.T.contiguous(), dy).float(), "dW")
+    _same(db, dy.double().sum(0).float(), "db")
