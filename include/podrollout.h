@@ -349,7 +349,7 @@ int block8_pack_weights(void *hip_stream, const pr_block8_layer *layer, const fl
  * x_kind PR_B8_BLOCKS: x codes, x_scale scale bytes (ldx is not read); else x [P rows, ldx] plain rows, which go through the
  * rule of the blocks on their way in.  y_kind likewise.  bias [P, out] fp32, or NULL.
  * (y in bf16 or blocks: products of 8 bits, whose sums of eight neighbours keep 13 bits below the largest product, 1.5e-5 of
- * the results in the 2-norm; y in fp32: fp32 sums of the exact products.  tanh is off by at most 1e-6 of its value in fp32,
+ * the sum of magnitudes; y in fp32: fp32 sums of the exact products, which block8_quantize makes blocks of.  tanh is off by at most 1e-6 of its value in fp32,
  * 3.1e-5 in bf16, 1e-5 in a block with no sum of 1/2 or more, and 2^-22 in other blocks, before that rounding.) */
 int block8_linear(void *hip_stream, const pr_block8_layer *layer, int32_t x_kind, const void *x, const uint8_t *x_scale,
                   int64_t ldx, const void *packed, const float *bias, int32_t y_kind, void *y, uint8_t *y_scale, int64_t ldy);
@@ -357,7 +357,10 @@ int block8_linear(void *hip_stream, const pr_block8_layer *layer, int32_t x_kind
 /* Gradients of the layer from its checkpoints: x and (tanh only, else NULL) y as blocks.  With dy [P rows, lddy] (fp32 or
  * bf16) the gradient of the outputs and Y the values of y's blocks:
  *   g = bf16(fl32(dy fl32(1 - Y^2))), or bf16(dy) without tanh;   dx = g W^T;   dW = X^T g;   db = sum over rows of g
- * (the rounding to blocks is passed straight through; g is the one rounding of gradients).  dx [P rows, lddx] of dx_kind, or
+ * (the rounding to blocks is passed straight through; g is the one rounding of gradients).  Y has four significant bits, so units
+ * count as saturated early: |tanh z| of 31/32 and more (|z| from 2.07 on) is stored as 1, with no gradient, where the true factor
+ * is up to 0.062; from 1/2 to there Y is off by up to 1/32 and the factor by up to 1/16.  A learner whose units live there keeps
+ * that layer's outputs plain, multiplies dy by 1 - y^2 itself and calls this for the layer without tanh.  dx [P rows, lddx] of dx_kind, or
  * NULL; dW [P, in, out], db [P, out] fp32.  Sums run in a fixed order.  rows = 0 gives zeros.
  * workspace: device, 256-byte aligned, block8_workspace_bytes of it: a size that serves any call of this layer with up to
  * `rows` rows (0 bytes and NULL are fine for none). */

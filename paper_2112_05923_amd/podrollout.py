@@ -666,7 +666,8 @@ def block8_workspace(w: Weights8, rows: int, device) -> torch.Tensor:
 
 def block8_linear_grads(dy: torch.Tensor, x: Blocks8, w: Weights8, y: Optional[Blocks8] = None, dx=None, workspace=None):
     """(dx, dW, db) of block8_linear from its checkpoints.  y: the layer's outputs (tanh), None for a layer without activation;
-    dx: torch.bfloat16, torch.float32, a tensor to write to, or None where the inputs need no gradient."""
+    dx: torch.bfloat16, torch.float32, a tensor to write to, or None where the inputs need no gradient.  y's codes of four bits
+    store |tanh| of 31/32 and more as 1: those units get no gradient (from plain outputs p: dy * (1 - p * p), and y=None)."""
     lead, rows, device = w.lead, dy.shape[-2], w.device
     ins, outs = lead + (rows, w.in_dim), lead + (rows, w.out_dim)
     dk, dp, lddy, _ = _plain_rows(dy, "dy", outs)
