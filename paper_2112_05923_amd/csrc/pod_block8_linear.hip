@@ -35,8 +35,8 @@ __global__ __launch_bounds__(256) void linear_kernel(Product a) {
 
 // Few rows: the weights are what has to be read, and many compute units have to read them.  A workgroup of sixteen wavefronts
 // has 32 rows x 32 features (128 where they become blocks, which share a maximum), the blocks of inputs dealt to its wavefronts,
-// whose sums meet in LDS.  Bound: latency, a launch and three round trips (1 row of 3001 inputs in fp32 to 1024 outputs 9.1 us,
-// 48 rows of 301 in bf16 to 512 5.8 us).
+// whose sums meet in LDS.  Bound: latency, a launch and three round trips (1 row of 3001 inputs in fp32 to 1024 outputs 9 us, on
+// 32 compute units; 48 rows of 301 in bf16 to 512 6 us).  Gradients as the rows spill 14 (bf16) and 36 (fp32) registers.
 template <int SRC, bool IN8, int OUT>
 __global__ __launch_bounds__(1024) void linear_few_kernel(Product a) {
   constexpr int kTiles = OUT == PR_B8_BLOCKS ? 4 : 1, kSplits = 16 / kTiles, kPitch = 65;
@@ -299,11 +299,13 @@ __device__ inline void multiply_resident(f32x16 (&acc)[4], const u32x4 *w, uint3
 // two rows.  A wavefront owns 32 rows at a time, with their codes in registers for all feature blocks; a block's registers take
 // the next rows' codes as soon as the last feature block is through with them.  Two wavefronts share a SIMD.  Workgroups for
 // the other features of the same rows (`slabs`) are on the same XCD at the same time.  262144 x 512 x 512, blocks to blocks:
-// 97 us, 1.4 PFLOP/s and 2.8 TB/s; matrix and vector pipe (tanh: two transcendentals an entry) are busy 36 % of the time each,
-// mostly one after the other in a wavefront.
+// 97 to 104 us, 1.4 PFLOP/s and 2.8 TB/s; matrix and vector pipe (tanh: two transcendentals an entry) are busy 36 % of the time
+// each, mostly one after the other in a wavefront.
 // Heads of up to 16 TILES outputs have them in the first TILES tiles of their one block (64 further ones, of the lanes above
 // 32, are zeros that come along); the other tiles are left out, of the products, of LDS and of the activation: 262144 x 512 x 30
-// to fp32 79 -> 48 us.
+// to fp32 79 -> 47 us, 3.3 TB/s.  One workgroup lives on a compute unit, by its share of the rows, and 256 registers are not
+// enough for four blocks of inputs to fp32: 51, 42 and 23 of them are spilled with four tiles, two and one, 22 MB of writes beside
+// the 31 of that result; with one tile 144 bytes a lane of an array lie in memory for any number of inputs.
 constexpr int kResidentWaves = 8, kResidentRows = 32, kResidentBytes = 131072;
 constexpr int kHead = kBlock + 4;  // floats per block of features in LDS: 128 biases, the scale bytes of its weights, the tickets
 
@@ -446,7 +448,7 @@ hipError_t launch_resident(hipStream_t st, int32_t P, const Product &a) {
 // refilled as soon as they are in registers.  Rows and results go between memory and LDS in whole lines: 16 rows x 4 pieces of
 // 16 bytes take a compute unit 100 cycles an instruction, 8 rows x 128 bytes a fifth.  Two workgroups live on a compute unit.
 // The feature blocks of the same rows follow each other on one XCD, whose L2 then has the rows.  65536 x 1024 x 1024, blocks to
-// bf16: 90 us, 1.5 PFLOP/s, matrix pipe busy 39 %; what is left are the barriers and the way out of 128 features at a time.
+// bf16: 92 us, 1.5 PFLOP/s, matrix pipe busy 38 %; what is left are the barriers and the way out of 128 features at a time.
 constexpr int kTilesRows = 256;
 constexpr int kStageBytes = 16384, kRowsBytes = 64 * kBlock;
 
@@ -553,13 +555,13 @@ __global__ __launch_bounds__(256, 2) void linear_tiles_kernel(Product a, int32_t
   for (int t = 0; t < 2; ++t) finish_lines<OUT>(acc[t], a, row0 + 32 * t, ob, lane, own[wave]);
 }
 
-// Plain rows, many of them.  A workgroup encodes 128 rows, a block of inputs at a time, once for up to four blocks of features:
-// eight lanes share a row (8 rows x 128 bytes an instruction: whole lines), the codes go to LDS, where every wavefront reads the
-// rows it multiplies.  A wavefront has one block of features and 32 TILES rows; its weights come from L2 straight into
+// Plain rows, many of them.  A workgroup encodes 128 rows, a block of inputs at a time, for up to four blocks of features (fp32
+// results; two for bf16 and blocks, so that rows are encoded twice for 512 features): eight lanes share a row (8 rows x 128 bytes
+// an instruction: whole lines), the codes go to LDS, where every wavefront reads the rows it multiplies.  A wavefront has one block of features and 32 TILES rows; its weights come from L2 straight into
 // registers, half a block of inputs ahead, and nobody else in the workgroup but the wavefront with its other rows wants them.
 // One barrier a block; rows are requested a block ahead.  131009 rows of 301 in fp32 to 512 features in blocks: 160 (every
-// wavefront encoding its own rows for its block of features, a lane a row) -> 128 us; vector pipe busy 38 %, matrix pipe 9 %:
-// 250 registers leave a workgroup of eight wavefronts alone on a compute unit, with nobody beside its round trips (a workgroup
+// wavefront encoding its own rows for its block of features, a lane a row) -> 128 us, where the bytes take 45; vector pipe busy
+// 38 %, matrix pipe 9 %: 250 registers leave a workgroup of eight wavefronts alone on a compute unit, with nobody beside its round trips (a workgroup
 // that goes on to its next tile, whose rows it requests early, spills and is slower: 150 us).
 constexpr int kPlainRows = 128;
 
@@ -725,8 +727,10 @@ hipError_t launch_plain(hipStream_t st, int32_t P, const Product &a) {
 // (they are the products' operand as they stand), and takes them through all inputs, whose weights pass through LDS, 32 KiB (a
 // block of either side) at a time and one ahead, for eight wavefronts.  With more than 512 outputs a wavefront needs a SIMD's
 // registers for itself.  Where rows alone do not fill the compute units the inputs are dealt to several workgroups too.
-// 131072 x 512 x 512 in bf16: 115 us, 600 TFLOP/s, of which the bytes (335 MB) take 65 and the products 27 at their peaks: all
-// workgroups live at once, and form g, multiply and store in step.
+// 131072 x 512 x 512 in bf16: 101 to 105 us, 670 TFLOP/s, where the bytes (335 MB) take 67 and the products 28 alone.  240
+// registers leave one workgroup on a compute unit, so its 512 go in two rounds, each of which forms g, multiplies and stores in step.
+// 65537 x 512 x 30: 28.5 us, where the bytes take 15: 140 registers leave one on a compute unit there too, and the last of 257, of
+// a single row, has a round of its own.
 template <class T, int OUT, int NB>
 __global__ __launch_bounds__(NB <= 4 ? 512 : 256, NB <= 4 ? 2 : 1) void input_grads_kernel(Product a, int32_t slab_blocks) {
   constexpr int kWaves = NB <= 4 ? 8 : 4, kPart = kWideTileBytes / kWaves;

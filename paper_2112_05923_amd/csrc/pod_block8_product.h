@@ -169,11 +169,13 @@ __device__ inline void load_operand(Operand<IN8> &o, const Product &a, int64_t r
 }
 
 // 32 features x 32 rows.  In 8 bits an instruction has 64 inputs, at twice the rate, and its sum of eight neighbouring products
-// keeps 13 bits below the largest of them (what it adds up behind that is fp32): 1.5e-5 of the result, measured, for results
-// that are rounded to bf16 or 8 bits (2e-3 and 3e-2).  Blocks show it where a sum lies that near a border between two codes:
-// 2-norm of the difference 7e-4 of the results, beside the 2.6e-2 that their own rounding is off.  Decoded to bf16 the products and sums are fp32's.
-// (32 x 32 tiles: 16 x 16 x 128 reads twice the registers for the same work and reaches 3490 TFLOP/s where this one has 4280
-// with a wavefront to each SIMD.)
+// keeps 13 bits below the largest of them (what it adds up behind that is fp32): at most 1.5e-5 of the sum of magnitudes on random
+// numbers, 1.5e-6 in the mean, for results that are rounded to bf16 or 8 bits (1.3e-3 and 2e-2 in the 2-norm).  Against the
+// unrounded result they are as far off as with fp32 sums, to four digits (bf16) and six (blocks); 6e-4 of the codes, whose sums lie
+// next to a border between two, are the neighbouring ones, 7e-4 of the results in the 2-norm.  Decoded to bf16 the products and
+// sums are fp32's, at half the rate: 262144 x 512 x 512 with its restore 169 -> 228 us, 65536 x 1024 x 1024 85 -> 122.
+// (32 x 32 tiles: 16 x 16 x 128 reads twice the registers for the same work and reaches 3870 TFLOP/s where this one has 4940
+// with a wavefront to each SIMD and its operands in registers.)
 template <int SEL>
 __device__ inline void multiply8(f32x16 &c, const i32x8 &w, uint32_t w_scale, const i32x8 &x, uint32_t x_scale) {
   c = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w, x, c, 0, 0, SEL, (int)w_scale, SEL, (int)x_scale);
