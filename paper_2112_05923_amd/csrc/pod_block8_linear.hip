@@ -299,11 +299,11 @@ __device__ inline void multiply_resident(f32x16 (&acc)[4], const u32x4 *w, uint3
 // two rows.  A wavefront owns 32 rows at a time, with their codes in registers for all feature blocks; a block's registers take
 // the next rows' codes as soon as the last feature block is through with them.  Two wavefronts share a SIMD.  Workgroups for
 // the other features of the same rows (`slabs`) are on the same XCD at the same time.  262144 x 512 x 512, blocks to blocks:
-// 97 to 104 us, 1.4 PFLOP/s and 2.8 TB/s; matrix and vector pipe (tanh: two transcendentals an entry) are busy 36 % of the time
+// 95 to 104 us, 1.4 PFLOP/s and 2.8 TB/s; matrix and vector pipe (tanh: two transcendentals an entry) are busy 36 % of the time
 // each, mostly one after the other in a wavefront.
 // Heads of up to 16 TILES outputs have them in the first TILES tiles of their one block (64 further ones, of the lanes above
 // 32, are zeros that come along); the other tiles are left out, of the products, of LDS and of the activation: 262144 x 512 x 30
-// to fp32 79 -> 47 us, 3.3 TB/s.  One workgroup lives on a compute unit, by its share of the rows, and 256 registers are not
+// to fp32 79 -> 48 us, 3.4 TB/s.  One workgroup lives on a compute unit, by its share of the rows, and 256 registers are not
 // enough for four blocks of inputs to fp32: 51, 42 and 23 of them are spilled with four tiles, two and one, 22 MB of writes beside
 // the 31 of that result; with one tile 144 bytes a lane of an array lie in memory for any number of inputs.
 constexpr int kResidentWaves = 8, kResidentRows = 32, kResidentBytes = 131072;
@@ -727,9 +727,9 @@ hipError_t launch_plain(hipStream_t st, int32_t P, const Product &a) {
 // (they are the products' operand as they stand), and takes them through all inputs, whose weights pass through LDS, 32 KiB (a
 // block of either side) at a time and one ahead, for eight wavefronts.  With more than 512 outputs a wavefront needs a SIMD's
 // registers for itself.  Where rows alone do not fill the compute units the inputs are dealt to several workgroups too.
-// 131072 x 512 x 512 in bf16: 101 to 105 us, 670 TFLOP/s, where the bytes (335 MB) take 67 and the products 28 alone.  240
+// 131072 x 512 x 512 in bf16: 101 to 110 us, 650 TFLOP/s, where the bytes (335 MB) take 67 and the products 28 alone.  240
 // registers leave one workgroup on a compute unit, so its 512 go in two rounds, each of which forms g, multiplies and stores in step.
-// 65537 x 512 x 30: 28.5 us, where the bytes take 15: 140 registers leave one on a compute unit there too, and the last of 257, of
+// 65537 x 512 x 30: 29 us, where the bytes take 15: 140 registers leave one on a compute unit there too, and the last of 257, of
 // a single row, has a round of its own.
 template <class T, int OUT, int NB>
 __global__ __launch_bounds__(NB <= 4 ? 512 : 256, NB <= 4 ? 2 : 1) void input_grads_kernel(Product a, int32_t slab_blocks) {
